@@ -155,14 +155,16 @@ struct Row {
 // which order like the values; infinities and NaN come last).  The quotient
 // 127 y / top is formed as y c times 1 / (top f) with one correction, so a value
 // halfway between two steps (which 127 y, exact for bfloat16 y, can be) comes
-// out halfway and goes to the even step.  f = 2^64 lifts rows whose reciprocal would overflow.
+// out halfway and goes to the even step.  f is 1 for rows between 2^-64 and 2^64, 2^64 below (whose
+// reciprocal would overflow) and 2^-64 above (where 127 y would, from 2.68e36 on, and
+// the reciprocal would be subnormal); what the latter makes subnormal is far below half a step.
 struct Quant {
     float c, inv, top, scale;
     __device__ __forceinline__ explicit Quant(uint32_t bits)
     {
         const bool ok = bits < 0x7f800000u;
         const float t = ok ? __uint_as_float(bits) : 0.f;
-        const float f = t < 5.42101086e-20f ? 18446744073709551616.f : 1.f;   // 2^-64, 2^64
+        const float f = t < 0x1p-64f ? 0x1p64f : t > 0x1p64f ? 0x1p-64f : 1.f;
         c = 127.f * f;
         top = t * f;
         inv = t > 0.f ? 1.f / top : 0.f;
