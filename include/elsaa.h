@@ -363,7 +363,8 @@ int elsaa_quantize_rows(const elsaa_quant_desc* desc, const void* X, int8_t* Q, 
  * transpose of elsaa_gemm's B), 8-bit two's complement; the sums are exact
  * 32-bit integers, scaled in float32 and rounded once to c_dtype.  C is plain (ldc) or
  * head-major (c_heads > 0, seq) as in elsaa_gemm, with any power of two >= 8 as head
- * width.  Requirements: 1 <= M, N <= 2^30, 1 <= K <= 131071 (the largest whose sums fit 32 bits), lda, ldb
+ * width.  Requirements: 1 <= M, N <= 2^30, 1 <= K <= 131071 (the largest whose sums fit 32 bits), fewer
+ * than 2^24 tiles of C (256 x 256 where K is a multiple of 16 and at least 128, else 128 x 128), lda, ldb
  * multiples of 16 (bytes), A and B 16-byte aligned, C aligned to its element; K need not be a multiple of
  * anything (bytes between K and the next multiple of 16 are read and ignored).
  * Long sums with few output tiles are split over workgroups whose integer

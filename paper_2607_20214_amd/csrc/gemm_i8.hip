@@ -547,9 +547,11 @@ __global__ __launch_bounds__(256) void gemm_i8_reduce_kernel(IArgs a)
 }
 
 constexpr int kRowsMax = 64;           // tokens that gemm_i8_rows_kernel takes
+constexpr int64_t kGridThreads = (int64_t)1 << 32;      // a launch has fewer threads in a dimension
 
 struct Plan {
     bool rows;
+    bool fits;                         // there are tiles that one launch holds
     int nj;                            // large tiles of 32 nj channels; 0: 128 x 128
     int tiles_m, tiles_n, splits, kper;
     size_t ws_bytes;
@@ -559,7 +561,9 @@ Plan plan_of(const elsaa_gemm_i8_desc* d)
 {
     auto parts = [](int64_t n, int64_t per) { return (n + per - 1) / per; };
     Plan p = {};
-    p.rows = d->M <= kRowsMax;
+    // (a workgroup of 256 threads for 16 channels; tiles take the rest)
+    p.rows = d->M <= kRowsMax && parts(d->N, 16) * 256 < kGridThreads;
+    p.fits = p.rows;
     const int64_t ktiles = parts(d->K, BKB);
     p.splits = 1;
     if (!p.rows) {
@@ -587,6 +591,8 @@ Plan plan_of(const elsaa_gemm_i8_desc* d)
         for (int nj : {0, 4, 6, 8}) {
             if (nj && (d->K < BKB || d->K % 16 != 0)) continue;
             const int64_t tiles = parts(d->M, nj ? big::BT : BM) * parts(d->N, nj ? 32 * nj : BN), fill = nj ? 256 : 512;
+            if (tiles * kThreads >= kGridThreads) continue;
+            p.fits = true;
             // at least four K-tiles a split, at most one round of workgroups
             int64_t most = tiles < fill ? fill / tiles : 1;
             if (most > ktiles / 4) most = ktiles / 4;
@@ -618,9 +624,12 @@ int validate(const elsaa_gemm_i8_desc* d)
     if (d->K > kMaxK) return api_fail(ELSAA_ERR_UNSUPPORTED, "K must be <= %d (got %d)", kMaxK, d->K);
     if (d->c_dtype != ELSAA_F32 && d->c_dtype != ELSAA_BF16)
         return api_fail(ELSAA_ERR_INVALID_ARG, "unknown c_dtype %d", d->c_dtype);
-    if (((int64_t)d->M + BM - 1) / BM * (((int64_t)d->N + BN - 1) / BN) > (1 << 30))
-        return api_fail(ELSAA_ERR_UNSUPPORTED, "M x N is too large (%d x %d)", d->M, d->N);
     return ELSAA_OK;
+}
+
+int too_large(const elsaa_gemm_i8_desc* d)
+{
+    return api_fail(ELSAA_ERR_UNSUPPORTED, "M x N is too large (%d x %d)", d->M, d->N);
 }
 
 int check_operand(const char* name, const void* p, int K, int64_t ld)
@@ -647,7 +656,9 @@ int elsaa_gemm_i8_workspace_bytes(const elsaa_gemm_i8_desc* d, size_t* bytes)
     const int rc = validate(d);
     if (rc) return rc;
     if (!bytes) return api_fail(ELSAA_ERR_INVALID_ARG, "bytes is NULL");
-    *bytes = plan_of(d).ws_bytes;
+    const Plan p = plan_of(d);
+    if (!p.fits) return too_large(d);
+    *bytes = p.ws_bytes;
     return ELSAA_OK;
 }
 
@@ -683,6 +694,7 @@ int elsaa_gemm_i8(const elsaa_gemm_i8_desc* d, const int8_t* A, const float* a_s
         while ((1 << a.C.dh_shift) < dh) ++a.C.dh_shift;
     }
     const Plan p = plan_of(d);
+    if (!p.fits) return too_large(d);
     if (p.ws_bytes > 0) {
         if (!workspace) return api_fail(ELSAA_ERR_INVALID_ARG, "workspace is NULL (%zu bytes needed)", p.ws_bytes);
         if (workspace_bytes < p.ws_bytes)
