@@ -362,44 +362,49 @@ __global__ __launch_bounds__(kThreads, T::bytes == 4 ? 1 : COLS == 128 ? 2 : D =
 
 // Slots of segment states -> states before each segment; the last sum is the
 // state behind the last token.  Eight slots are requested at a time: their
-// addresses do not depend on the sum.
+// addresses do not depend on the sum.  A workgroup takes 1024 values of a
+// state, and further ones where there are more than the launch has workgroups
+// (a launch holds 2^24 of them, fewer than 2^20 states of 128 x 128).
+constexpr int kScanGroups = 1 << 16;
 template <int D>
-__global__ __launch_bounds__(256) void decay_scan_kernel(DecayArgs a, int count)
+__global__ __launch_bounds__(256) void decay_scan_kernel(DecayArgs a, int count, int total)
 {
     const StateRole& ro = a.st[blockIdx.y];
     constexpr int PER = D * D / 4 / 256;               // workgroups a (b, h)
-    const int bh = blockIdx.x / PER, e = (blockIdx.x - bh * PER) * 256 + threadIdx.x;
-    const int b = bh / a.H, h = bh - b * a.H;
-    const int len = length_of(a, b);
-    const float lg = log2_decay(a, h);
-    f32x4* slot = (f32x4*)(ro.slots + (int64_t)bh * (a.nseg + 1) * D * D) + e;
-    constexpr int64_t step = D * D / 4;
-    // (row, column) of the first of this thread's four values (rows row .. row + 3)
-    const int lane = e & 63, blk = e >> 6;
-    const int row = 16 * (blk % (D / 16)) + 4 * (lane >> 4), col = 16 * (blk / (D / 16)) + (lane & 15);
-    const int64_t user = (int64_t)bh * D * D + row * D + col;
-    f32x4 run = {0, 0, 0, 0};
-    if (ro.init) {
+    for (int wg = blockIdx.x; wg < total; wg += gridDim.x) {
+        const int bh = wg / PER, e = (wg - bh * PER) * 256 + threadIdx.x;
+        const int b = bh / a.H, h = bh - b * a.H;
+        const int len = length_of(a, b);
+        const float lg = log2_decay(a, h);
+        f32x4* slot = (f32x4*)(ro.slots + (int64_t)bh * (a.nseg + 1) * D * D) + e;
+        constexpr int64_t step = D * D / 4;
+        // (row, column) of the first of this thread's four values (rows row .. row + 3)
+        const int lane = e & 63, blk = e >> 6;
+        const int row = 16 * (blk % (D / 16)) + 4 * (lane >> 4), col = 16 * (blk / (D / 16)) + (lane & 15);
+        const int64_t user = (int64_t)bh * D * D + row * D + col;
+        f32x4 run = {0, 0, 0, 0};
+        if (ro.init) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) run[r] = ro.init[user + r * D];
-        slot[0] = run;                                  // (`fin` may be `init`)
-    }
-    constexpr int U = 8;
-    for (int s0 = 0; s0 < count; s0 += U) {
-        f32x4 own[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) own[u] = slot[min(s0 + u + 1, count) * step];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int s = s0 + u;
-            if (s >= count) break;
-            run = run * power(lg, min(max(len - s * a.seg_len, 0), a.seg_len)) + own[u];
-            if (s + 1 < a.nseg) slot[(s + 1) * step] = run;
+            for (int r = 0; r < 4; ++r) run[r] = ro.init[user + r * D];
+            slot[0] = run;                                  // (`fin` may be `init`)
         }
-    }
-    if (ro.fin) {
+        constexpr int U = 8;
+        for (int s0 = 0; s0 < count; s0 += U) {
+            f32x4 own[U];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) ro.fin[user + r * D] = run[r];
+            for (int u = 0; u < U; ++u) own[u] = slot[min(s0 + u + 1, count) * step];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int s = s0 + u;
+                if (s >= count) break;
+                run = run * power(lg, min(max(len - s * a.seg_len, 0), a.seg_len)) + own[u];
+                if (s + 1 < a.nseg) slot[(s + 1) * step] = run;
+            }
+        }
+        if (ro.fin) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) ro.fin[user + r * D] = run[r];
+        }
     }
 }
 
@@ -699,7 +704,9 @@ hipError_t launch(const DecayArgs& a, int bh, int states, int outs, hipStream_t 
         else
             ELSAA_LAUNCH("decay_state", (decay_state_kernel<T, D, WIDE>), grid(items, states, WIDE), dim3(kThreads), 0, st, a, count,
                          items);
-        ELSAA_LAUNCH("decay_scan", decay_scan_kernel<D>, dim3(bh * (D * D / 1024), states), dim3(256), 0, st, a, count);
+        const int total = bh * (D * D / 1024);
+        ELSAA_LAUNCH("decay_scan", decay_scan_kernel<D>, dim3(total < kScanGroups ? total : kScanGroups, states), dim3(256), 0, st, a,
+                     count, total);
     }
     const int items = bh * a.nseg;
     if (narrow(items, outs, 256))
