@@ -40,7 +40,8 @@ from __future__ import annotations
 import torch
 
 from . import (Buffers, Config, DecayConfig, bwd, decay_bwd, decay_fwd, decay_step, decay_workspace_bytes, fwd, gemm,
-               gemm_i8, gemm_plan, gemm_workspace_bytes, quantize_rows, rms_norm_bwd, rms_norm_fwd, rms_norm_i8)
+               gemm_i8, gemm_plan, gemm_workspace_bytes, quantize_rows, rms_norm_bwd, rms_norm_fwd, rms_norm_i8,
+               rms_norm_workspace_bytes)
 
 
 class AttentionBlock:
@@ -149,7 +150,9 @@ class DecayBlock:
                  gemm_plan(self.out, W_O, trans_b=True, out=self.do), gemm_plan(self.o, self.out, trans_a=True, out=self.dW_O),
                  gemm_plan(self.dqkv, W_qkv, trans_b=True, out=self.dy),
                  gemm_plan(self.y, self.dqkv, trans_a=True, out=self.dW_qkv)]
-        ws = max([gemm_workspace_bytes(p) for p in plans] + [decay_workspace_bytes(cfg, True)])
+        # one workspace for all: the calls of a step follow each other on one stream
+        ws = max([gemm_workspace_bytes(p) for p in plans] +
+                 [decay_workspace_bytes(cfg, False), decay_workspace_bytes(cfg, True), rms_norm_workspace_bytes(B * N, dm)])
         self.ws = torch.empty(max(ws, 256), dtype=torch.uint8, device=dev)
 
     def _heads(self, t):
@@ -179,7 +182,8 @@ class DecayBlock:
                   out=self._heads(self.dqkv), workspace=self.ws)
         gemm(self.dqkv, self.W_qkv, trans_b=True, out=self.dy, workspace=self.ws)
         gemm(self.y, self.dqkv, trans_a=True, out=self.dW_qkv, workspace=self.ws)
-        rms_norm_bwd(self.s, self.norm_w, self.dy, dsum=ds, eps=self.eps, out=self.dx, out_dweight=self.dnorm_w)
+        rms_norm_bwd(self.s, self.norm_w, self.dy, dsum=ds, eps=self.eps, out=self.dx, out_dweight=self.dnorm_w,
+                     workspace=self.ws)
         return {"dx": self.dx, "dW_qkv": self.dW_qkv, "dW_O": self.dW_O, "dnorm_w": self.dnorm_w}
 
 
