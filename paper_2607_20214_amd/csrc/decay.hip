@@ -126,6 +126,16 @@ struct Rows {
     }
 };
 
+// Sign bits of the bfloat16 halves (of the float32 words) set where a value is
+// an infinity or NaN; the other bits mean nothing.
+template <class T>
+__device__ __forceinline__ uint32_t not_finite(uint4 v)
+{
+    constexpr uint32_t E = T::bytes == 2 ? 0x7f807f80u : 0x7f800000u, ONE = T::bytes == 2 ? 0x00800080u : 0x00800000u;
+    return ((v.x & E) + ONE) | ((v.y & E) + ONE) | ((v.z & E) + ONE) | ((v.w & E) + ONE);
+}
+template <class T> constexpr uint32_t kSigns = T::bytes == 2 ? 0x80008000u : 0x80000000u;
+
 // Q is kept in LDS with the four-element units 0 .. 7 of every 32 columns in
 // the order 0 4 1 5 2 6 3 7: the readout's operand of lane group g, columns 4 g .. and 16 + 4 g ..
 // (the state's rows as its accumulators hold them), is then 16 contiguous bytes.
@@ -408,9 +418,51 @@ __global__ __launch_bounds__(256) void decay_scan_kernel(DecayArgs a, int count,
     }
 }
 
+// The readout of a segment's rows from position t on, token by token, for
+// segments with an infinity or NaN among the values: in a chunk it would meet
+// the zeros of P in the rows before its token, and 0 x infinity is NaN.  The recurrence
+// from the segment's first token, float32 throughout, 1.2 to 1.8 us a token
+// (16 heads of 16384 x 128 with one NaN, segments of 512 tokens: 0.85 ms where the chunks alone take 0.12).  Thread (i, c): rows i, i + RT, .. of four columns, sums over the rows in `red`.
+template <class T, int D, int COLS>
+__device__ void decay_walk(const DecayArgs& a, const OutRole& ro, const float* slot, const float* first, const typename T::store_t* Q,
+                           const typename T::store_t* K, const typename T::store_t* V, typename T::store_t* O, int c0, float lg, int len,
+                           int t0, int t, int t1, f32x4* red)
+{
+    constexpr int CG = COLS / 4, RT = kThreads / CG;
+    const int c = threadIdx.x % CG, i = threadIdx.x / CG, col = c0 + 4 * c;
+    f32x4 s[D / RT];
+#pragma unroll
+    for (int j = 0; j < D / RT; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int row = i + j * RT, x = ro.trans ? col + e : row, y = ro.trans ? row : col + e;
+            s[j][e] = slot ? slot[slot_index<D>(x, y)] : first ? first[x * D + y] : 0.f;
+        }
+    const float before = power(lg, 1 - ro.shift), behind = power(lg, ro.shift);
+    for (int x = t0; x < t1; ++x) {
+        const int64_t row = (int64_t)token_of(x, len, ro.rev) * D;
+        const f32x4 v = load4<T>(V + row + 4 * c);
+        f32x4 o = {0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < D / RT; ++j) {
+            s[j] = s[j] * before + v * (ro.s_tok * T::load(K[row + i + j * RT]));
+            o += s[j] * T::load(Q[row + i + j * RT]);
+            s[j] *= behind;
+        }
+        if (x < t) continue;
+        __syncthreads();
+        red[i * CG + c] = o;
+        __syncthreads();
+        if (i == 0) {
+            for (int j = 1; j < RT; ++j) o += red[j * CG + c];
+            store4<T>(O + row + 4 * c, o * ro.s_out);
+        }
+    }
+}
+
 // Readout of one segment, COLS columns.
 template <class T, int D, int COLS>
-__global__ __launch_bounds__(kThreads, T::bytes == 4 ? 1 : D == 128 ? 2 : 3) void decay_out_kernel(DecayArgs a, int items)
+__global__ __launch_bounds__(kThreads, T::bytes == 4 ? 128 / D : D == 128 ? 2 : 3) void decay_out_kernel(DecayArgs a, int items)
 {
     using RK = Rows<T, D, D>;
     constexpr int NV = COLS / 64;
@@ -422,6 +474,7 @@ __global__ __launch_bounds__(kThreads, T::bytes == 4 ? 1 : D == 128 ? 2 : 3) voi
     using F = typename T::frag_t;
     __shared__ __attribute__((aligned(16))) S Qs[TK::elems(kChunk)], Ks[TK::elems(kChunk)], Vs[TV::elems(kChunk)];
     __shared__ __attribute__((aligned(16))) S Ps[TP::elems(kChunk)];
+    __shared__ int special;                            // a value of V is an infinity or NaN
     const OutRole& ro = a.out[blockIdx.y];
     int item, part;
     if (!item_of<D / COLS>(items, item, part)) return;
@@ -443,6 +496,7 @@ __global__ __launch_bounds__(kThreads, T::bytes == 4 ? 1 : D == 128 ? 2 : 3) voi
             stg16(O + (int64_t)(z0 + x / TV::CPR) * D + x % TV::CPR * TV::EPC, make_uint4(0, 0, 0, 0));
     }
     if (t0 >= t1) return;
+    if (threadIdx.x == 0) special = 0;
 
     const int last = t0 + (t1 - 1 - t0) / kChunk * kChunk;
     uint4 qr[RK::P], kr[RK::P], vr[RV::P];
@@ -479,11 +533,16 @@ __global__ __launch_bounds__(kThreads, T::bytes == 4 ? 1 : D == 128 ? 2 : 3) voi
     const float keep = power(lg, kChunk);
 
     // One chunk; whole ones carry no conditions, so that the waits for the
-    // next rows do not wait for this chunk's stores as well.
+    // next rows do not wait for this chunk's stores as well.  False, and
+    // nothing written, where the values are not all finite.
     auto chunk = [&](int t, auto whole) {
         constexpr bool WHOLE = decltype(whole)::value;
         const int n = WHOLE ? kChunk : t1 - t;
+        uint32_t nf = 0;
+#pragma unroll
+        for (int j = 0; j < RV::P; ++j) nf |= not_finite<T>(vr[j]);
         __syncthreads();
+        if (nf & kSigns<T>) special = 1;
         put_q<T, D>(Qs, qr, n);
         RK::put(Ks, kr, n);
         RV::put(Vs, vr, n);
@@ -540,7 +599,9 @@ __global__ __launch_bounds__(kThreads, T::bytes == 4 ? 1 : D == 128 ? 2 : 3) voi
         for (int m = 0; m < NV; ++m)
 #pragma unroll
             for (int qt = 0; qt < 4; ++qt) o[m][qt] *= fq[qt];
+        const int stop = special;
         __syncthreads();
+        if (__builtin_amdgcn_readfirstlane(stop)) return false;
         // O^T += V^T P^T
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
@@ -565,10 +626,16 @@ __global__ __launch_bounds__(kThreads, T::bytes == 4 ? 1 : D == 128 ? 2 : 3) voi
         }
         // (a short chunk is the last one)
         if (WHOLE) update_state<T, D, T::kSplit ? 2 : 1>(st, Ks, Vs, keep, wt);
+        return true;
     };
     int t = t0;
-    for (; t + kChunk <= t1; t += kChunk) chunk(t, std::true_type{});
-    if (t < t1) chunk(t, std::false_type{});
+    bool done = true;
+    for (; done && t + kChunk <= t1; t += done ? kChunk : 0) done = chunk(t, std::true_type{});
+    if (done && t < t1) done = chunk(t, std::false_type{});
+    if (!done)
+        decay_walk<T, D, COLS>(a, ro, seg || ro.slot0 ? ro.slots + ((int64_t)bh * (a.nseg + 1) + seg) * D * D : nullptr,
+                               ro.first ? ro.first + (int64_t)bh * D * D : nullptr, Q, K, V + COLS * part, O, COLS * part, lg, len, t0, t,
+                               t1, (f32x4*)Qs);
 }
 
 // One token: state columns [16 blockIdx.y, +16) of one (b, h).  Thread (i, c):
