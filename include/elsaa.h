@@ -395,8 +395,8 @@ int elsaa_gemm_i8(const elsaa_gemm_i8_desc* desc, const int8_t* A, const float* 
  *
  * lengths: int32 [B] on the device or NULL (every sequence has N tokens);
  * values are clamped to 0 .. N.  Tokens at and behind a sequence's length are not
- * read; their rows of O are left as they were, their rows of dQ, dK, dV are
- * set to zero.
+ * read; their rows of O are left as they were, or set to zero where zero_tail is
+ * not 0, their rows of dQ, dK, dV are set to zero.
  *
  * elsaa_decay_fwd: state is S_0 (NULL: zero); state_out, when not NULL, receives S behind the last
  * token (it may be `state` itself).
@@ -418,6 +418,7 @@ typedef struct {
     float scale;
     int64_t q_batch, k_batch, v_batch, o_batch;         /* o_batch: O and dO */
     int64_t dq_batch, dk_batch, dv_batch;
+    int32_t zero_tail;                                  /* forward with lengths: rows of O behind them become zero */
 } elsaa_decay_desc;
 
 int elsaa_decay_workspace_bytes(const elsaa_decay_desc* desc, int pass, size_t* bytes);

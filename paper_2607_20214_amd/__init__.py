@@ -77,7 +77,8 @@ class _GemmI8Desc(C.Structure):
 
 class _DecayDesc(C.Structure):
     _fields_ = [("B", C.c_int32), ("H", C.c_int32), ("N", C.c_int32), ("d_h", C.c_int32), ("dtype", C.c_int32),
-                ("scale", C.c_float)] + [(n + "_batch", C.c_int64) for n in ("q", "k", "v", "o", "dq", "dk", "dv")]
+                ("scale", C.c_float)] + [(n + "_batch", C.c_int64) for n in ("q", "k", "v", "o", "dq", "dk", "dv")] + [
+                    ("zero_tail", C.c_int32)]
 
 
 @dataclasses.dataclass
@@ -830,18 +831,20 @@ def decay_workspace_bytes(cfg: DecayConfig, backward: bool = False) -> int:
 
 
 def decay_fwd(cfg: DecayConfig, q, k, v, log_decay, state=None, lengths=None, out=None, out_state=None,
-              want_state=True, workspace: Optional[torch.Tensor] = None):
+              want_state=True, workspace: Optional[torch.Tensor] = None, zero_tail=False):
     """(o, state): S_t = exp(log_decay) S_{t-1} + k_t v_t^T, o_t = scale q_t^T S_t
     over N tokens from `state` (None: zero); the returned state [B, H, d_h, d_h]
     float32 is the one behind the last token (None unless want_state).
     q, k, v are [B, H, N, d_h], each sequence contiguous (head ranges of one
-    projection buffer will do); lengths int32 [B] shortens sequences: rows of o behind them are not written."""
+    projection buffer will do); lengths int32 [B] shortens sequences: rows of o behind them are not written,
+    or set to zero with zero_tail."""
     dev = q.device
     if out is None:
         out = torch.empty(cfg.B, cfg.H, cfg.N, cfg.d_h, dtype=cfg.torch_dtype, device=dev)
     if out_state is None and want_state:
         out_state = torch.empty(cfg.B, cfg.H, cfg.d_h, cfg.d_h, dtype=torch.float32, device=dev)
     d = _decay_desc(cfg, dev, q=q, k=k, v=v, o=out)
+    d.zero_tail = int(zero_tail)
     _decay_common(cfg, dev, log_decay, lengths, state=state, out_state=out_state)
     ws = _workspace(workspace, _decay_workspace(d, False), dev)
     _launch(dev, load().elsaa_decay_fwd, C.byref(d), _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(state),

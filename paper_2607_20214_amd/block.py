@@ -163,12 +163,9 @@ class DecayBlock:
         """(out, s): the block's output and the residual stream x + residual."""
         _, s = rms_norm_fwd(x, self.norm_w, residual=residual, eps=self.eps, out=self.y, out_sum=self.s)
         gemm(self.y, self.W_qkv, out=self.qkv, workspace=self.ws)
-        if self.lengths is not None:
-            # rows behind a sequence's length are not written by the attention:
-            # zeros there keep them out of the output and of dW_O
-            self.o.zero_()
+        # (zeros behind a sequence's length keep those rows out of the output and of dW_O)
         decay_fwd(self.cfg, *self._heads(self.qkv), self.log_decay, lengths=self.lengths, out=self.o, want_state=False,
-                  workspace=self.ws)
+                  workspace=self.ws, zero_tail=True)
         gemm(self.o, self.W_O, out=self.out, workspace=self.ws)
         return self.out, s
 
@@ -227,9 +224,8 @@ class DecayServer:
         cfg = DecayConfig(self.B, self.H, N, self.d_h)
 
         def attention(q, k, v):
-            out = torch.zeros(self.B, self.H, N, self.d_h, dtype=torch.bfloat16, device=x.device) if lengths is not None else None
-            return decay_fwd(cfg, q, k, v, self.log_decay, state=self.state if cont else None, lengths=lengths, out=out,
-                             out_state=self.state)[0]
+            return decay_fwd(cfg, q, k, v, self.log_decay, state=self.state if cont else None, lengths=lengths,
+                             out_state=self.state, zero_tail=True)[0]
 
         return self._attend(x, residual, N, attention)
 

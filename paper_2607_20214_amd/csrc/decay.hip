@@ -846,6 +846,7 @@ int elsaa_decay_fwd(const elsaa_decay_desc* d, const void* Q, const void* K, con
     a.st[0] = StateRole{K, V, batch[1], batch[2], 0, 0, 1.f, (float*)workspace, state, state_out};
     a.out[0] = OutRole{Q, K, V, O, batch[0], batch[1], batch[2], batch[3], 0, 0, 1.f, a.tau, nullptr, nullptr, 0, 0};
     set_first(a.out[0], a.st[0], p.nseg > 1 || state_out);
+    a.zero_tail = lengths && d->zero_tail;
     const hipError_t e = launch_any(d, a, 1, 1, stream);
     return e == hipSuccess ? ELSAA_OK : api_hip_fail(e, "decay forward");
 }
