@@ -249,7 +249,7 @@ def _run_own(c, t):
         return (out, t["s"]) if c["mode"] == "norm" else (out,)
     if c["mode"] == "fwd":
         return E.decay_fwd(t["cfg"], t["q"], t["k"], t["v"], t["g"], state=t.get("s0"), lengths=t.get("len"),
-                           out=t["o"], out_state=t["s1"], workspace=t["ws"])
+                           out=t["o"], out_state=t["s1"], workspace=t["ws"], zero_tail=True)
     if c["mode"] == "bwd":
         return E.decay_bwd(t["cfg"], t["q"], t["k"], t["v"], t["g"], t["do"], state=t.get("s0"),
                            lengths=t.get("len"), out=(t["dq"], t["dk"], t["dv"]), workspace=t["ws"])[:3]
