@@ -308,16 +308,16 @@ int elsaa_gemm(const elsaa_gemm_desc* desc, const void* A, const void* B, void* 
  *              scale = max_j |y_j| / 127, q_j = y_j / scale rounded to
  *              nearest, ties to even.  A row of zeros has scale 0; a row with
  *              an infinity or NaN has scale NaN and q 0.
- * `sum` may be x or the residual itself, y (storage type) may be x, each at
- * the same row stride: a row is read before it is written.  Buffers must not
- * overlap otherwise.
+ * `sum` may be x or the residual itself, y (storage type) may be x or the residual,
+ * each at the same row stride: a row is read before it is written.  Another stride, and
+ * sum and y at one address, are refused; buffers must not overlap otherwise.
  *
  * elsaa_rms_norm_bwd is the gradient at the stored s (argument X, ldx), from
  * dY (ldy) and, when not NULL, the residual stream's own gradient dS (ldr):
  *     dx_j = rho (w_j dy_j - s_j rho^2 mean_i(w_i dy_i s_i)) + ds_j   (dX, lds)
  *     dw_j = sum over rows of dy_j s_j rho                         (float32)
- * dX is the gradient of x and of the residual alike; it may be dS or dY
- * itself at the same stride.  dweight may be NULL.  dw is summed over the workgroups'
+ * dX is the gradient of x and of the residual alike; it may be dS, dY or X
+ * itself at the same stride (another is refused).  dweight may be NULL.  dw is summed over the workgroups'
  * partial sums in `workspace` (elsaa_rms_norm_workspace_bytes; 0 without dweight need
  * not be passed) in a fixed order, so it is the same from run to run.
  * Requirements: rows >= 1, 1 <= cols <= 16384, pointers aligned to their

@@ -628,7 +628,7 @@ def rms_norm_fwd(x, weight, residual=None, eps=1e-6, out=None, out_sum=None):
     """(y, s): s = x + residual, y = s / sqrt(mean(s^2) + eps) * weight over the
     last dimension.  x and residual bfloat16 or float32, weight float32; y and
     s in x's type, s None without a residual (unless out_sum is given).
-    out_sum may be x or residual, out may be x."""
+    out_sum and out may each be x or residual, but not the same one."""
     _gpu("x", x)
     if out is None:
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device)

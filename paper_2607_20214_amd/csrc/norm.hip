@@ -515,6 +515,15 @@ int check_rows(const char* name, const void* p, int64_t ld, int cols, int elem)
     return ELSAA_OK;
 }
 
+// an output at an input's address: its rows must be the input's
+int check_in_place(const char* name, const void* out, int64_t ldo, const void* in, int64_t ldi, int64_t rows)
+{
+    if (out && out == in && ldo != ldi && rows > 1)
+        return api_fail(ELSAA_ERR_INVALID_ARG, "%s is written over an input with another row stride (%lld, %lld)", name, (long long)ldo,
+                        (long long)ldi);
+    return ELSAA_OK;
+}
+
 template <class T, int V>
 void launch_fwd(const NormArgs& a, bool i8, hipStream_t st)
 {
@@ -572,6 +581,12 @@ int elsaa_rms_norm_fwd(const elsaa_norm_desc* d, const void* X, const void* resi
         return rc;
     if (!aligned(weight, 4) || (i8 && !aligned(scale, 4)))
         return api_fail(ELSAA_ERR_INVALID_ARG, "weight and scale must be 4-byte aligned");
+    if (sum == Y) return api_fail(ELSAA_ERR_INVALID_ARG, "sum and Y must be different buffers");
+    if (i8 && (Y == X || Y == residual)) return api_fail(ELSAA_ERR_INVALID_ARG, "8-bit Y must not be X or the residual");
+    if ((rc = check_in_place("sum", sum, d->lds, X, d->ldx, d->rows)) ||
+        (rc = check_in_place("sum", sum, d->lds, residual, d->ldr, d->rows)) || (rc = check_in_place("Y", Y, d->ldy, X, d->ldx, d->rows)) ||
+        (rc = check_in_place("Y", Y, d->ldy, residual, d->ldr, d->rows)))
+        return rc;
     NormArgs a = {};
     a.x = X; a.r = residual; a.w = weight; a.s = sum; a.y = Y; a.scale = scale;
     a.rows = d->rows; a.ldx = d->ldx; a.ldr = d->ldr; a.lds = d->lds; a.ldy = d->ldy;
@@ -606,6 +621,9 @@ int elsaa_rms_norm_bwd(const elsaa_norm_desc* d, const void* X, const float* wei
         return rc;
     if (!aligned(weight, 4) || !aligned(dweight, 4) || !aligned(workspace, 4))
         return api_fail(ELSAA_ERR_INVALID_ARG, "weight, dweight and workspace must be 4-byte aligned");
+    if ((rc = check_in_place("dX", dX, d->lds, X, d->ldx, d->rows)) || (rc = check_in_place("dX", dX, d->lds, dY, d->ldy, d->rows)) ||
+        (rc = check_in_place("dX", dX, d->lds, dS, d->ldr, d->rows)))
+        return rc;
     const int64_t parts = bwd_blocks(d->rows, d->cols);
     const size_t need = (size_t)parts * d->cols * sizeof(float);
     if (dweight && workspace_bytes < need)
