@@ -767,7 +767,7 @@ hipError_t launch(const DecayArgs& a, int bh, int states, int outs, hipStream_t 
     if (count > 0) {
         const int items = bh * count;
         if (narrow(items, states, 320))
-            ELSAA_LAUNCH("decay_state", (decay_state_kernel<T, D, 64>), grid(items, states, 64), dim3(kThreads), 0, st, a, count, items);
+            ELSAA_LAUNCH("decay_state_half", (decay_state_kernel<T, D, 64>), grid(items, states, 64), dim3(kThreads), 0, st, a, count, items);
         else
             ELSAA_LAUNCH("decay_state", (decay_state_kernel<T, D, WIDE>), grid(items, states, WIDE), dim3(kThreads), 0, st, a, count,
                          items);
@@ -777,7 +777,7 @@ hipError_t launch(const DecayArgs& a, int bh, int states, int outs, hipStream_t 
     }
     const int items = bh * a.nseg;
     if (narrow(items, outs, 256))
-        ELSAA_LAUNCH("decay_out", (decay_out_kernel<T, D, 64>), grid(items, outs, 64), dim3(kThreads), 0, st, a, items);
+        ELSAA_LAUNCH("decay_out_half", (decay_out_kernel<T, D, 64>), grid(items, outs, 64), dim3(kThreads), 0, st, a, items);
     else
         ELSAA_LAUNCH("decay_out", (decay_out_kernel<T, D, WIDE>), grid(items, outs, WIDE), dim3(kThreads), 0, st, a, items);
     return hipGetLastError();
