@@ -730,10 +730,11 @@ int elsaa_gemm_i8(const elsaa_gemm_i8_desc* d, const int8_t* A, const float* a_s
         return e == hipSuccess ? ELSAA_OK : api_hip_fail(e, "gemm_i8 launch");
     }
     const dim3 grid((unsigned)(p.tiles_m * p.tiles_n * p.splits));
+    const char* big_name = p.nj == 8 ? "gemm_i8_256x256" : p.nj == 6 ? "gemm_i8_256x192" : "gemm_i8_256x128";
 #define ELSAA_I8_BIG(NJ)                                                                                                      \
     do {                                                                                                                      \
-        if (bf16) ELSAA_LAUNCH("gemm_i8_large", (big::gemm_i8_big_kernel<true, NJ>), grid, dim3(kThreads), 0, stream, a);     \
-        else ELSAA_LAUNCH("gemm_i8_large", (big::gemm_i8_big_kernel<false, NJ>), grid, dim3(kThreads), 0, stream, a);         \
+        if (bf16) ELSAA_LAUNCH(big_name, (big::gemm_i8_big_kernel<true, NJ>), grid, dim3(kThreads), 0, stream, a);            \
+        else ELSAA_LAUNCH(big_name, (big::gemm_i8_big_kernel<false, NJ>), grid, dim3(kThreads), 0, stream, a);                \
     } while (0)
     if (p.nj == 8) ELSAA_I8_BIG(8);
     else if (p.nj == 6) ELSAA_I8_BIG(6);
