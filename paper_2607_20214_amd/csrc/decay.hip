@@ -22,7 +22,8 @@
 // segment's own state, a scan adds up the states before each segment, and the
 // readout walks a segment's 64-token chunks with the state in registers.
 // States, scores and outputs are float32; operands of the matrix cores are
-// in the storage type.
+// in the storage type, those formed here (weighted values, scores, states) as sums of two or three
+// bfloat16 parts, so that nothing but a row's output is rounded to 8 bits.
 #include "common.hpp"
 #include "elsaa.h"
 #include "internal.hpp"
@@ -431,13 +432,15 @@ __device__ void decay_walk(const DecayArgs& a, const OutRole& ro, const float* s
     constexpr int CG = COLS / 4, RT = kThreads / CG;
     const int c = threadIdx.x % CG, i = threadIdx.x / CG, col = c0 + 4 * c;
     f32x4 s[D / RT];
+    auto load = [&](auto at) {
 #pragma unroll
-    for (int j = 0; j < D / RT; ++j)
+        for (int j = 0; j < D / RT; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int row = i + j * RT, x = ro.trans ? col + e : row, y = ro.trans ? row : col + e;
-            s[j][e] = slot ? slot[slot_index<D>(x, y)] : first ? first[x * D + y] : 0.f;
-        }
+            for (int e = 0; e < 4; ++e) s[j][e] = at(ro.trans ? col + e : i + j * RT, ro.trans ? i + j * RT : col + e);
+    };
+    if (slot) load([&](int x, int y) { return slot[slot_index<D>(x, y)]; });
+    else if (first) load([&](int x, int y) { return first[x * D + y]; });
+    else load([](int, int) { return 0.f; });
     const float before = power(lg, 1 - ro.shift), behind = power(lg, ro.shift);
     for (int x = t0; x < t1; ++x) {
         const int64_t row = (int64_t)token_of(x, len, ro.rev) * D;
@@ -473,7 +476,13 @@ __global__ __launch_bounds__(kThreads, T::bytes == 4 ? 128 / D : D == 128 ? 2 : 
     using S = typename T::store_t;
     using F = typename T::frag_t;
     __shared__ __attribute__((aligned(16))) S Qs[TK::elems(kChunk)], Ks[TK::elems(kChunk)], Vs[TV::elems(kChunk)];
-    __shared__ __attribute__((aligned(16))) S Ps[TP::elems(kChunk)];
+    // Scores and the state are operands in two bfloat16 parts (float32: one), so
+    // that a row is as exact as its own rounding: error against exact sums 1.66e-3
+    // of a bfloat16 tensor's norm, and 2.35e-3 with one part of each.  (16 heads of 16384 x
+    // 128: 118 us, and 113 with one part; backward 304 and 265; d 64, 64 heads of 4096: 51 and 47,
+    // backward 100 and 91.)
+    constexpr int PARTS = T::kSplit ? 2 : 1;
+    __shared__ __attribute__((aligned(16))) S Ps[PARTS][TP::elems(kChunk)];
     __shared__ int special;                            // a value of V is an infinity or NaN
     const OutRole& ro = a.out[blockIdx.y];
     int item, part;
@@ -500,17 +509,28 @@ __global__ __launch_bounds__(kThreads, T::bytes == 4 ? 128 / D : D == 128 ? 2 : 
 
     const int last = t0 + (t1 - 1 - t0) / kChunk * kChunk;
     uint4 qr[RK::P], kr[RK::P], vr[RV::P];
-    auto fetch = [&](int t) {
+    auto fetch_q = [&](int t) {
+        RK rk;
+        t = min(t, last);
+        rk.at(t, t1 - t, len, ro.rev);
+        rk.get(Q, qr);
+    };
+    auto fetch_kv = [&](int t) {
         RK rk;
         RV rv;
         t = min(t, last);
         rk.at(t, t1 - t, len, ro.rev);
         rv.at(t, t1 - t, len, ro.rev, COLS * part);
-        rk.get(Q, qr);
         rk.get(K, kr);
         rv.get(V, vr);
     };
-    fetch(t0);
+    // At 128 columns a workgroup 256 registers do not hold the next rows and both
+    // parts of the state: K and V are requested behind its readout, and what depends on the
+    // lane alone is formed in every chunk (all at its start, with registers
+    // spilled: 16 heads of 16384 x 128 155 us, backward 371; at 64 columns 2 % slower).
+    constexpr bool LATE = T::bytes == 2;
+    fetch_q(t0);
+    fetch_kv(t0);
     State<D, NV> st;
     const int c0 = COLS * part + 16 * NV * w;
     if (seg || ro.slot0) st.load(ro.slots + ((int64_t)bh * (a.nseg + 1) + seg) * D * D, c0, ro.trans);
@@ -546,8 +566,12 @@ __global__ __launch_bounds__(kThreads, T::bytes == 4 ? 128 / D : D == 128 ? 2 : 
         put_q<T, D>(Qs, qr, n);
         RK::put(Ks, kr, n);
         RV::put(Vs, vr, n);
-        fetch(t + kChunk);
+        fetch_q(t + kChunk);
+        if (!LATE) fetch_kv(t + kChunk);
         __syncthreads();
+        int lane = threadIdx.x & 63;
+        if (LATE) asm volatile("" : "+v"(lane));
+        const int g = lane >> 4, i = lane & 15;
         // scores of this wave's 16 rows with rows 16 kt .. on, and a tile of zeros where
         // the readout, in steps of 32 rows, reads past the diagonal
 #pragma unroll
@@ -567,7 +591,13 @@ __global__ __launch_bounds__(kThreads, T::bytes == 4 ? 128 / D : D == 128 ? 2 : 
 #pragma unroll
                 for (int r = 0; r < 4; ++r) p[r] = kt == w && i >= 4 * g + r ? p[r] * fp[kt][r] : 0.f;
             }
-            put4<T>(&Ps[TP::row(16 * w + i) + 16 * kt + 4 * g], p);
+            const int at = TP::row(16 * w + i) + 16 * kt + 4 * g;
+            put4<T>(&Ps[0][at], p);
+            if constexpr (PARTS == 2) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) p[r] -= (float)(__bf16)p[r];
+                put4<T>(&Ps[1][at], p);
+            }
         }
         // O^T = S^T Q^T, rows of O^T in this wave's columns
         f32x4 o[NV][4];
@@ -577,7 +607,7 @@ __global__ __launch_bounds__(kThreads, T::bytes == 4 ? 128 / D : D == 128 ? 2 : 
             for (int qt = 0; qt < 4; ++qt) o[m][qt] = f32x4{0, 0, 0, 0};
 #pragma unroll
         for (int s = 0; s < D / 32; ++s) {
-            F sf[NV];
+            F sf[PARTS][NV];
 #pragma unroll
             for (int m = 0; m < NV; ++m) {
                 float x[8];
@@ -586,19 +616,23 @@ __global__ __launch_bounds__(kThreads, T::bytes == 4 ? 128 / D : D == 128 ? 2 : 
                     x[r] = st.s[2 * s][m][r];
                     x[4 + r] = st.s[2 * s + 1][m][r];
                 }
-                sf[m] = T::pack(x);
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p) sf[p][m] = take_part<T>(x, p + 1 < PARTS);
             }
 #pragma unroll
             for (int qt = 0; qt < 4; ++qt) {
                 const F q = TK::row8(Qs, 16 * qt + i, 32 * s + 8 * g);
 #pragma unroll
-                for (int m = 0; m < NV; ++m) o[m][qt] = T::mma(sf[m], q, o[m][qt]);
+                for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+                    for (int m = 0; m < NV; ++m) o[m][qt] = T::mma(sf[p][m], q, o[m][qt]);
             }
         }
 #pragma unroll
         for (int m = 0; m < NV; ++m)
 #pragma unroll
             for (int qt = 0; qt < 4; ++qt) o[m][qt] *= fq[qt];
+        if (LATE) fetch_kv(t + kChunk);
         const int stop = special;
         __syncthreads();
         if (__builtin_amdgcn_readfirstlane(stop)) return false;
@@ -610,9 +644,12 @@ __global__ __launch_bounds__(kThreads, T::bytes == 4 ? 128 / D : D == 128 ? 2 : 
             for (int m = 0; m < NV; ++m) v[m] = TV::col8(Vs, 32 * ks, 16 * NV * w + 16 * m);
 #pragma unroll
             for (int qt = 2 * ks; qt < 4; ++qt) {
-                const F p = TP::row8(Ps, 16 * qt + i, 32 * ks + 8 * g);
 #pragma unroll
-                for (int m = 0; m < NV; ++m) o[m][qt] = T::mma(v[m], p, o[m][qt]);
+                for (int p = 0; p < PARTS; ++p) {
+                    const F pf = TP::row8(Ps[p], 16 * qt + i, 32 * ks + 8 * g);
+#pragma unroll
+                    for (int m = 0; m < NV; ++m) o[m][qt] = T::mma(v[m], pf, o[m][qt]);
+                }
             }
         }
 #pragma unroll
@@ -625,7 +662,7 @@ __global__ __launch_bounds__(kThreads, T::bytes == 4 ? 128 / D : D == 128 ? 2 : 
             }
         }
         // (a short chunk is the last one)
-        if (WHOLE) update_state<T, D, T::kSplit ? 2 : 1>(st, Ks, Vs, keep, wt);
+        if (WHOLE) update_state<T, D, PARTS>(st, Ks, Vs, keep, wt);
         return true;
     };
     int t = t0;
