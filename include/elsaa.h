@@ -299,7 +299,7 @@ int elsaa_gemm(const elsaa_gemm_desc* desc, const void* A, const void* B, void* 
  * (ld >= cols); the weight is float32 [cols].  Sums and the norm are float32
  * whatever the storage type, and y is formed from the unrounded s.
  * (Squares are summed as they are: where a row's sum of them passes 3.4e38, rho and
- * the finite y are 0.)
+ * the finite y are 0, and the row has no meaningful gradient.)
  *
  * elsaa_rms_norm_fwd writes s to `sum` in the storage type (NULL: not kept;
  * without a residual s is x) and y as y_dtype says:
@@ -361,7 +361,8 @@ int elsaa_quantize_rows(const elsaa_quant_desc* desc, const void* X, int8_t* Q, 
  *     C_ij = a_scale_i b_scale_j sum_k A_ik B_jk
  * A [M, K] (row stride lda), B [N, K] (row stride ldb: a row for each channel, the
  * transpose of elsaa_gemm's B), 8-bit two's complement; the sums are exact
- * 32-bit integers, scaled in float32 and rounded once to c_dtype.  C is plain (ldc) or
+ * 32-bit integers, scaled in float32 (by a_scale, then b_scale: infinite where the sum times
+ * a_scale passes 3.4e38) and rounded once to c_dtype.  C is plain (ldc) or
  * head-major (c_heads > 0, seq) as in elsaa_gemm, with any power of two >= 8 as head
  * width.  Requirements: 1 <= M, N <= 2^30, 1 <= K <= 131071 (the largest whose sums fit 32 bits), fewer
  * than 2^24 tiles of C (256 x 256 where K is a multiple of 16 and at least 128, else 128 x 128), lda, ldb

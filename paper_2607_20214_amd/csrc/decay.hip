@@ -479,8 +479,8 @@ __global__ __launch_bounds__(kThreads, T::bytes == 4 ? 128 / D : D == 128 ? 2 : 
     // Scores and the state are operands in two bfloat16 parts (float32: one), so
     // that a row is as exact as its own rounding: error against exact sums 1.66e-3
     // of a bfloat16 tensor's norm, and 2.35e-3 with one part of each.  (16 heads of 16384 x
-    // 128: 118 us, and 113 with one part; backward 304 and 265; d 64, 64 heads of 4096: 51 and 47,
-    // backward 100 and 91.)
+    // 128: 131 us, and 122 with one part, backward 270 and 242; 64 heads of 4096 x 64: 54 and 50,
+    // backward 110 and 102.)
     constexpr int PARTS = T::kSplit ? 2 : 1;
     __shared__ __attribute__((aligned(16))) S Ps[PARTS][TP::elems(kChunk)];
     __shared__ int special;                            // a value of V is an infinity or NaN
@@ -527,7 +527,7 @@ __global__ __launch_bounds__(kThreads, T::bytes == 4 ? 128 / D : D == 128 ? 2 : 
     // At 128 columns a workgroup 256 registers do not hold the next rows and both
     // parts of the state: K and V are requested behind its readout, and what depends on the
     // lane alone is formed in every chunk (all at its start, with registers
-    // spilled: 16 heads of 16384 x 128 155 us, backward 371; at 64 columns 2 % slower).
+    // spilled: the same 16 heads 154 us, backward 330).
     constexpr bool LATE = T::bytes == 2;
     fetch_q(t0);
     fetch_kv(t0);
@@ -719,14 +719,14 @@ struct Plan {
     size_t slots;            // floats of one set of slots
 };
 
-// Segments of whole chunks.  More segments fill the chip
-// better and cost states written, scanned and read.  Forward (16 heads of 128):
-// two workgroups a compute unit from eight chunks a segment on (16K tokens: 116
-// us with 512 workgroups, 125 with 256), one below (4K: 47 with 256, 54 with 512).
-// Backward: its three readouts in one round of what is resident (16K: 255 us with 3 x 160
-// workgroups, 282 with 3 x 512; 128 heads of 2K: 180 with one segment a head, no
-// state pass, and 240 with four), three a compute unit at 64 in bfloat16 (64
-// heads of 4K: 92 with four segments, 111 with two).  Float32 at 128 takes two workgroups a
+// Segments of whole chunks.  More segments fill the chip better and cost
+// states written, scanned and read.  Forward: two workgroups a compute unit from eight chunks a
+// segment on (64 heads of 4096 x 64: 54 us with 512 workgroups, 64 with 256; 16 heads of 16384 x
+// 128: 127 and 126), one below (16 heads of 4096 x 128: 46 with 256, 56 with 512).
+// Backward: its three readouts in one round of what is resident (16 heads of 16384 x 128: 269 us with
+// 3 x 160 workgroups, 290 with 3 x 512; 128 heads of 2048: 209 with one segment a head, no
+// state pass, and 266 with four), three a compute unit at 64 in bfloat16 (64
+// heads of 4096: 111 with four segments, 139 with two).  Float32 at 128 takes two workgroups a
 // segment.
 Plan plan_of(const elsaa_decay_desc* d, bool backward)
 {
@@ -788,9 +788,9 @@ int check_workspace(const void* ws, size_t have, size_t need)
 // A workgroup takes all columns of a state where that is 64 or (bfloat16) 128,
 // or 64 of the 128.  Each wave reads the whole of Q and of K from LDS whatever its
 // width, and LDS is what halves are slower by where the chip is full (16K
-// tokens, 16 heads of 128: readout 68 us against 60).  Where it is not (up to one
+// tokens, 16 heads of 128: 134 us against 122).  Where it is not (up to one
 // workgroup a compute unit in the readout, 1.25 in the state pass) they bring twice the
-// waves (4K tokens: forward 47.5 -> 43.4 us, backward 84 -> 80).  In float32 only
+// waves (4K tokens: forward 50 -> 46 us, backward 94 -> 91).  In float32 only
 // tiles of 64 columns fit LDS.
 template <class T, int D>
 hipError_t launch(const DecayArgs& a, int bh, int states, int outs, hipStream_t st)

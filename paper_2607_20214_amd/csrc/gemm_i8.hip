@@ -47,9 +47,8 @@ constexpr int kThreads = 256;
 // 28-31, and the same 32 lanes on): rows 0-3 and 12-15 of one chunk and 4-11 of
 // its neighbour.  With the chunks of a row exchanged by the row pair's number these
 // 256 bytes lie in 64 different banks; padding of 16 bytes a row or a row pair leaves two of them
-// in one bank, which adds half to the read.  16384 x 6144 x 2048, padded against exchanged:
-// 260 and 251 us with evenly spread values; 224 either way with normal ones
-// quantised, where the card's power sets the pace.
+// in one bank, which adds half to the read (1000 x 2048 x 2048: 19.9 us padded, 19.0 exchanged;
+// 16384 x 6144 x 2048: 226 either way, the matrix cores and the card's power set its pace).
 __device__ __forceinline__ constexpr int lds_at(int r, int c) { return r * BKB + 16 * (c ^ ((r >> 1) & 7)); }
 constexpr int kGroupM = 8;
 
@@ -568,15 +567,14 @@ Plan plan_of(const elsaa_gemm_i8_desc* d)
     p.splits = 1;
     if (!p.rows) {
         // Estimated microseconds of a tile size and split count, a round being
-        // the workgroups resident at once (256 large tiles or 512 small ones).
-        // Measured a K-tile and for a round's first loads and last stores: 1.8 + 12.5
-        // us in rounds of 256 x 256 tiles (16384 x 6144 x 2048: 259 us, 8002 x
-        // 2048 x 2048: 41), 1.62 + 8.3 at 192 channels (4096 x 6144 x 2048, two whole
-        // rounds: 67 against 75 in one and a half of the largest), 1.18 + 7 at
-        // 128 (4096 x 2048 x 2048, one round: 26 against 36), 1.25 + 9 for the small
-        // tiles and three quarters of that where they fill at most half the
-        // chip (2048 x 2048 x 2048: 21.7 against 22.3 and more).  Splitting K costs a
-        // launch and the partial sums' way to memory and back.
+        // the workgroups resident at once (256 large tiles or 512 small ones): a
+        // cost for each K-tile and one for a round's first loads and last stores, fitted to
+        // products of one to six rounds.  Small tiles take three quarters where they fill at most half the
+        // chip; splitting K costs a launch and the partial sums' way to memory and back.
+        // The lines this draws, measured (us with 256 x 256, 256 x 192, 256 x 128 and 128 x 128 tiles):
+        // 16384 x 6144 x 2048 226, 250, 270, 298; 8002 x 2048 x 2048 39, 59, 47, 53;
+        // 4096 x 6144 x 2048 70, 64, 69, 80; 4096 x 2048 x 2048 34, 32, 24.5, 29; 2048 x 2048 x 2048 32, 29,
+        // 21.0, 20.3.
         auto estimate = [&](int nj, int64_t tiles, int splits) {
             const int fill = nj ? 256 : 512;
             const int64_t per = parts(ktiles, splits);
