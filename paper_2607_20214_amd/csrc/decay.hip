@@ -422,8 +422,9 @@ __global__ __launch_bounds__(256) void decay_scan_kernel(DecayArgs a, int count,
 // The readout of a segment's rows from position t on, token by token, for
 // segments with an infinity or NaN among the values: in a chunk it would meet
 // the zeros of P in the rows before its token, and 0 x infinity is NaN.  The recurrence
-// from the segment's first token, float32 throughout, 1.2 to 1.8 us a token
-// (16 heads of 16384 x 128 with one NaN, segments of 512 tokens: 0.85 ms where the chunks alone take 0.12).  Thread (i, c): rows i, i + RT, .. of four columns, sums over the rows in `red`.
+// from the segment's first token, float32 throughout, 1.2 to 1.8 us a token (16
+// heads of 16384 x 128 with one NaN, segments of 512 tokens: 0.85 ms where the chunks alone
+// take 0.12).  Thread (i, c): rows i, i + RT, .. of four columns, sums over the rows in `red`.
 template <class T, int D, int COLS>
 __device__ void decay_walk(const DecayArgs& a, const OutRole& ro, const float* slot, const float* first, const typename T::store_t* Q,
                            const typename T::store_t* K, const typename T::store_t* V, typename T::store_t* O, int c0, float lg, int len,
